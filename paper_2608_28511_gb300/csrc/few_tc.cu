@@ -39,6 +39,7 @@ constexpr int kRows = 128;  // weight rows of a tile
 constexpr int kK = 64;      // depth of a block: 128 bytes, one swizzle row
 constexpr int kABytes = kRows * kK * 2;
 constexpr int kMaxStages = 12;
+constexpr float kMaxBf16 = 0x1.fep127f;
 constexpr int kXchg = 2 * 64 * 17 * 4;  // two buffers of 64 up rows x 16 columns, padded
 
 struct TcArgs {
@@ -423,10 +424,16 @@ __global__ void __launch_bounds__(kThreads, 1) few_layer_tc_kernel(const __grid_
             for (int i = 0; i < 16; ++i) {
               if (i >= n) break;
               const float z = v[i] * sigmoid_rn(v[i]) * xb[(q * 32 + lane) * 17 + i];
-              const bf16 hi = __float2bfloat16_rn(z);
               const int64_t at = (int64_t)(it.r0 + c0 + i) * a.F + f;
-              act[at] = hi;
-              if (p.terms == 2) act[at + low] = __float2bfloat16_rn(z - __bfloat162float(hi));
+              if (p.terms == 2) {
+                // the first term stays finite, so that the second is z's rest where z
+                // rounds to infinity, and infinity or NaN where z is
+                const bf16 hi = __float2bfloat16_rn(fminf(fmaxf(z, -kMaxBf16), kMaxBf16));
+                act[at] = hi;
+                act[at + low] = __float2bfloat16_rn(z - __bfloat162float(hi));
+              } else {
+                act[at] = __float2bfloat16_rn(z);
+              }
             }
           }
           buf ^= 1;
