@@ -174,7 +174,11 @@ __global__ void __launch_bounds__(256) ckpt_dprob_kernel(const float* __restrict
   dprob[r] = s;
 }
 
-size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+// The tensor maps in the workspace want 128-byte alignment, callers owe 16: the
+// carve-up starts at the next multiple of 256, and the size leaves room for that.
+constexpr size_t kWsAlign = 256;
+size_t up256(size_t v) { return (v + kWsAlign - 1) & ~(kWsAlign - 1); }
+char* ws_base(void* ws) { return reinterpret_cast<char*>(up256(reinterpret_cast<uintptr_t>(ws))); }
 
 // act of the forward pass; and the backward pass's rows of dy and x, dH, p act,
 // partial dprob sums and the two weight gradients' tensor maps.
@@ -194,7 +198,7 @@ Carve carve(const ShapeInfo& d) {
   w.part = w.act + up256(n * d.F * 2);
   w.maps0 = w.part + up256(n * w.parts * 4);
   w.maps1 = w.maps0 + up256(gemm_tc_group_scratch_bytes(d.E));
-  w.total = w.maps1 + up256(gemm_tc_group_scratch_bytes(d.E));
+  w.total = w.maps1 + up256(gemm_tc_group_scratch_bytes(d.E)) + kWsAlign - 1;
   return w;
 }
 
@@ -336,7 +340,7 @@ extern "C" int moe_expert_ffn_ckpt(const moe_shape_t* shape, const void* x_perm,
   if (ws_bytes < w.total) return MOE_ERR_WORKSPACE;
   Ctx c;
   CKPT_TRY(abi_device_ctx(stream, &c));
-  void* act = static_cast<char*>(ws) + w.act_f;
+  void* act = ckpt::ws_base(ws) + w.act_f;
   // GEMM-1, its epilogue: act = silu(g) u and the codes and scales of h, which
   // is never written in 16 bits
   GemmDesc g1 = ckpt::by_rows(Epi::SwigluFwdQ8, d, expert_offsets, x_perm, d.D, w1, 2 * (int64_t)d.F, false, h_q,
@@ -362,7 +366,7 @@ extern "C" int moe_expert_ffn_bwd_ckpt(const moe_shape_t* shape, const void* dy,
   if (ws_bytes < w.total) return MOE_ERR_WORKSPACE;
   Ctx c;
   CKPT_TRY(abi_device_ctx(stream, &c));
-  char* base = static_cast<char*>(ws);
+  char* base = ckpt::ws_base(ws);
   void *dy_rows = base + w.dy, *x_rows = base + w.x, *dh = base + w.dh, *act = base + w.act;
   float* part = reinterpret_cast<float*>(base + w.part);
   const DType ct = dw_dtype == MOE_BF16 ? DType::BF16 : DType::F32;
