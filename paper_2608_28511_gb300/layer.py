@@ -25,9 +25,10 @@ class LayerScratch:
     def __init__(self, shape: abi.MoeShape, device="cuda"):
         dev = torch.device(device)
         TK, D = shape.T * shape.K, shape.D
-        self.key = (shape.S, shape.GBS, shape.K, D, shape.E, shape.F, shape.H, dev.type)
         bf = lambda *n: torch.empty(*n, dtype=torch.bfloat16, device=dev)  # noqa: E731
         self.x_perm, self.y_perm, self.dx_perm = bf(TK, D), bf(TK, D), bf(TK, D)
+        # the device of the buffers, index included, however it was named
+        self.key = (shape.S, shape.GBS, shape.K, D, shape.E, shape.F, shape.H, self.x_perm.device)
         self.dprob_perm = torch.empty(TK, dtype=torch.float32, device=dev)
         self.ws_ckpt = torch.empty(abi.moe_ckpt_workspace_size(shape), dtype=torch.uint8, device=dev)
         self.ws = torch.empty(abi.moe_workspace_size(shape), dtype=torch.uint8, device=dev)
@@ -120,8 +121,9 @@ class MoeLayer:
         self.scratch = sc = None
         if checkpoint:
             self.scratch = sc = scratch or LayerScratch(self.shape, dev)
-            if sc.key != (S, GBS, K, D, E, F, H, dev.type):
-                raise ValueError(f"scratch of (S, GBS, K, D, E, F, H) = {sc.key}, not {(S, GBS, K, D, E, F, H)}")
+            key = (S, GBS, K, D, E, F, H, self.x.device)
+            if sc.key != key:
+                raise ValueError(f"scratch of (S, GBS, K, D, E, F, H, device) = {sc.key}, not {key}")
         self.h_q = e(TK, 2 * F, d=torch.int8) if sc else None
         self.h_scale = e(2 * F // 32, TK, d=f32) if sc else None
         self.x_perm = sc.x_perm if sc else None if self.gather else e(TK, D)
