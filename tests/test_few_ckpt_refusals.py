@@ -17,12 +17,14 @@ def L():
 
 
 def test_scratch_of_another_device(L):
-    """Two devices of one kind are two devices (meta tensors keep the index they are given)."""
+    """Two GPUs are two devices (tensors without memory, which keep the device they are made for)."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
     from paper_2608_28511_gb300.layer import LayerScratch, MoeLayer
     base = dict(S=64, GBS=1, K=2, D=128, E=8, F=64)
-    sc = LayerScratch(L.MoeShape.of(**base), "meta:0")
-    same = MoeLayer(**base, device="meta:0", checkpoint="int8", scratch=sc)
-    assert same.x_perm is sc.x_perm
-    for device in ("meta:1", "cpu"):
-        with pytest.raises(ValueError, match="scratch"):
-            MoeLayer(**base, device=device, checkpoint="int8", scratch=sc)
+    with FakeTensorMode(allow_non_fake_inputs=True):
+        sc = LayerScratch(L.MoeShape.of(**base), "cuda:0")
+        assert MoeLayer(**base, device="cuda:0", checkpoint="int8", scratch=sc).x_perm is sc.x_perm
+        for device in ("cuda:1", "cpu"):
+            with pytest.raises(ValueError, match="scratch"):
+                MoeLayer(**base, device=device, checkpoint="int8", scratch=sc)
