@@ -18,7 +18,6 @@ __device__ uint32_t g_status_word;
 
 namespace {
 
-constexpr int kMaxDevices = 64;
 std::mutex g_mu;
 uint32_t* g_status_ptr[kMaxDevices] = {};
 int g_num_sms[kMaxDevices] = {};

@@ -22,7 +22,6 @@ static __device__ __align__(256) int32_t g_dispatch_scratch[MOE_DISPATCH_NOALLOC
 
 namespace {
 
-constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mu;
 int32_t* g_scratch_ptr[kMaxDevices] = {};
 

@@ -496,17 +496,16 @@ cudaError_t launch_few_tc(const Ctx& c, const Args& a) {
   // than a quarter of the blocks, nothing is cut.
   const bool split = a.T <= kSplitT && 4 * a.K * std::min(a.F / 64, (a.D + kRows - 1) / kRows) <= c.num_sms;
   auto kernel = split ? few_layer_tc_kernel<true> : few_layer_tc_kernel<false>;
-  static int budgets[2][64] = {};  // by device (abi_device_ctx admits no more)
-  int& budget = budgets[split][c.device];
-  if (!budget) {
+  static PerDevice budgets[2];
+  int budget = 0;  // bytes of dynamic shared memory
+  const cudaError_t st = budgets[split].get(c.device, cudaSuccess, &budget, [&](int* v) {
     cudaFuncAttributes fa;
     cudaError_t e = cudaFuncGetAttributes(&fa, kernel);
     if (e != cudaSuccess) return e;
-    const int dyn = (227 * 1024 - (int)fa.sharedSizeBytes) & ~1023;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dyn);
-    if (e != cudaSuccess) return e;
-    budget = dyn;
-  }
+    *v = (227 * 1024 - (int)fa.sharedSizeBytes) & ~1023;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, *v);
+  });
+  if (st != cudaSuccess) return st;
   p.stages = std::min(kMaxStages, (budget - 1024 - kXchg) / stage_bytes) / p.nacc * p.nacc;
   const int64_t items = (int64_t)std::min(a.E, a.T * a.K) * std::max(a.F / 64, (a.D + kRows - 1) / kRows) *
                         (split ? kSplitParts : 1);

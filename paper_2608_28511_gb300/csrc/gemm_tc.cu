@@ -172,19 +172,21 @@ cudaError_t launch_inst(const Ctx& c, const Params& p, int64_t ub) {
   constexpr int kZW = (GROUP == 2 && GATHER == 0) ? 1 : 0;
   constexpr int kSmem = Cfg<BN, CG, sizeof(TC), EPI, kZW>::kSmem;
   constexpr int kThreads = Cfg<BN, CG, sizeof(TC), EPI, kZW>::kThreads;
-  static bool configured = false;
-  static int pairs = 0;
-  if (!configured) {
+  static PerDevice setup;
+  int pairs = 0;
+  const cudaError_t st = setup.get(c.device, cudaSuccess, &pairs, [&](int* v) {
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
+    *v = 0;
     if (CG == 2) {
       e = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 0);
       (void)e;
       cudaGetLastError();
-      pairs = max_pair_clusters(k, kSmem, kThreads);
+      *v = max_pair_clusters(k, kSmem, kThreads);
     }
-    configured = true;
-  }
+    return cudaSuccess;
+  });
+  if (st != cudaSuccess) return st;
   int np = pairs > 0 ? pairs : c.num_sms / 2;
   if (ub < np) np = (int)ub;
   cudaLaunchConfig_t cfg = {};

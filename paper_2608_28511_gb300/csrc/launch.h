@@ -6,6 +6,7 @@
 #include <stddef.h>
 
 #include "moe.h"
+#include "per_device.h"
 
 namespace moe {
 
