@@ -400,21 +400,65 @@ def moe_ckpt_workspace_size(shape: MoeShape) -> int:
     return n.value
 
 
+def _any(name, t, *_):
+    return _p(t)
+
+
+def _checked(fn):
+    """f(name, tensor, type, elements, width of the rows): the tensor's address, once it has these (a flat tensor
+    has no rows) and is on the current device, all of which the library cannot see.  With no type and number only
+    the device counts.  None and addresses pass."""
+    at = None
+
+    def f(name, t, kind, n, width=None):
+        nonlocal at
+        if t is None or isinstance(t, int):
+            return t
+        if n is not None and (t.dtype is not kind or t.numel() != n or
+                              (width is not None and t.size(-1) != width and t.dim() > 1)):
+            raise ValueError(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, not {n} elements" +
+                             (f" in rows of {width}" if width else "") + f" of {kind}")
+        dev = t.get_device()  # -1: not a GPU
+        if dev != at:
+            if dev < 0 or at is not None or dev != (_torch or _t()).cuda.current_device():
+                raise ValueError(f"{fn}: {name} is on {t.device}, not on the current device or the others'")
+            at = dev
+        if not t.is_contiguous():
+            raise ValueError(f"{fn}: {name} is not contiguous")
+        return t.data_ptr()
+
+    return f
+
+
 def moe_expert_ffn_ckpt(shape, x_perm, expert_offsets, w1, w2, h_q, h_scale, y_perm, ws, stream=None):
+    torch = _torch or _t()
+    TK, D, E, F, bf = shape.T * shape.K, shape.D, shape.E, shape.F, torch.bfloat16
+    p = _checked("moe_expert_ffn_ckpt") if shape.x_dtype == MOE_BF16 else _any  # the library refuses fp32
     _check("moe_expert_ffn_ckpt", lib().moe_expert_ffn_ckpt(
-        _shape(shape), _p(x_perm), _p(expert_offsets), _p(w1), _p(w2), _p(h_q), _p(h_scale), _p(y_perm), _p(ws),
-        _nbytes(ws), _stream(stream)))
+        _shape(shape), p("x_perm", x_perm, bf, TK * D, D), p("expert_offsets", expert_offsets, torch.int32, E + 1),
+        p("w1", w1, bf, 2 * E * F * D, D), p("w2", w2, bf, E * D * F, F), p("h_q", h_q, torch.int8, 2 * TK * F, 2 * F),
+        p("h_scale", h_scale, torch.float32, TK * F // 16, TK), p("y_perm", y_perm, bf, TK * D, D),
+        p("ws", ws, None, None), _nbytes(ws), _stream(stream)))
 
 
 def moe_expert_ffn_bwd_ckpt(shape, dy, x, prob_perm, row_of_slot, expert_offsets, h_q, h_scale, w1, w2, dx_perm, dw1,
                             dw2, dprob_perm, ws, stream=None):
     """dw1 and dw2 are both bf16 or both fp32."""
-    if dw1.dtype != dw2.dtype:
-        raise ValueError(f"dw1 is {dw1.dtype}, dw2 {dw2.dtype}")
+    dw = dw1.dtype
+    if dw != dw2.dtype:
+        raise ValueError(f"dw1 is {dw}, dw2 {dw2.dtype}")
+    torch = _torch or _t()
+    T, D, E, F = shape.T, shape.D, shape.E, shape.F
+    TK, n1, n2 = T * shape.K, 2 * E * F * D, E * D * F
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    p = _checked("moe_expert_ffn_bwd_ckpt") if shape.x_dtype == MOE_BF16 else _any
     _check("moe_expert_ffn_bwd_ckpt", lib().moe_expert_ffn_bwd_ckpt(
-        _shape(shape), _p(dy), _p(x), _p(prob_perm), _p(row_of_slot), _p(expert_offsets), _p(h_q), _p(h_scale),
-        _p(w1), _p(w2), _p(dx_perm), _rows_dtype(dw1), _p(dw1), _p(dw2), _p(dprob_perm), _p(ws), _nbytes(ws),
-        _stream(stream)))
+        _shape(shape), p("dy", dy, bf, T * D, D), p("x", x, bf, T * D, D), p("prob_perm", prob_perm, f32, TK),
+        p("row_of_slot", row_of_slot, i32, TK), p("expert_offsets", expert_offsets, i32, E + 1),
+        p("h_q", h_q, torch.int8, 2 * TK * F, 2 * F), p("h_scale", h_scale, f32, TK * F // 16, TK),
+        p("w1", w1, bf, n1, D), p("w2", w2, bf, n2, F), p("dx_perm", dx_perm, bf, TK * D, D), _rows_dtype(dw1),
+        p("dw1", dw1, dw, n1, D), p("dw2", dw2, dw, n2, F), p("dprob_perm", dprob_perm, f32, TK),
+        p("ws", ws, None, None), _nbytes(ws), _stream(stream)))
 
 
 def moe_few_workspace_size(shape: MoeShape) -> int:

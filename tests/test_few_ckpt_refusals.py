@@ -28,3 +28,49 @@ def test_scratch_of_another_device(L):
         for device in ("cuda:1", "cpu"):
             with pytest.raises(ValueError, match="scratch"):
                 MoeLayer(**base, device=device, checkpoint="int8", scratch=sc)
+
+
+def _ffn_args(device="cpu", T=6, K=2, D=64, E=4, F=128):
+    e = lambda *s, d=torch.bfloat16: torch.empty(*s, dtype=d, device=device)  # noqa: E731
+    n, i32, f32 = T * K, torch.int32, torch.float32
+    fwd = dict(x_perm=e(n, D), expert_offsets=e(E + 1, d=i32), w1=e(E, 2 * F, D), w2=e(E, D, F),
+               h_q=e(n, 2 * F, d=torch.int8), h_scale=e(2 * F // 32, n, d=f32), y_perm=e(n, D), ws=None)
+    bwd = dict(dy=e(T, D), x=e(T, D), prob_perm=e(n, d=f32), row_of_slot=e(T, K, d=i32),
+               **{k: fwd[k] for k in ("expert_offsets", "h_q", "h_scale", "w1", "w2")}, dx_perm=e(n, D),
+               dw1=e(E, 2 * F, D), dw2=e(E, D, F), dprob_perm=e(n, d=f32), ws=None)
+    return dict(S=T, GBS=1, K=K, D=D, E=E, F=F), fwd, bwd
+
+
+@pytest.mark.parametrize("which", ["forward", "backward"])
+def test_ckpt_ffn_tensors(L, which, monkeypatch):
+    """Every tensor of another type or size, and the scales as [rows, blocks], are refused by name."""
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    shape, fwd, bwd = _ffn_args()
+    s = L.MoeShape.of(**shape)
+    fn, args = (L.moe_expert_ffn_ckpt, fwd) if which == "forward" else (L.moe_expert_ffn_bwd_ckpt, bwd)
+    for k, t in args.items():
+        if t is None:
+            continue
+        bad = [t[:-1]] if t.dim() == 1 or k in ("dy", "x") else [t[:, :-1]]
+        if k not in ("dw1", "dw2"):  # fp32 or bf16
+            bad += [t.double(), t.long()]
+        if t.dim() > 1 and k != "row_of_slot":
+            bad.append(t.transpose(-1, -2).contiguous())
+        for b in bad:
+            with pytest.raises(ValueError, match=f"{k} is"):
+                fn(s, **{**args, k: b}, stream=0)
+
+
+@pytest.mark.parametrize("which", ["forward", "backward"])
+def test_ckpt_ffn_devices(L, which):
+    shape, fwd, bwd = _ffn_args()
+    s = L.MoeShape.of(**shape)
+    fn, args = (L.moe_expert_ffn_ckpt, fwd) if which == "forward" else (L.moe_expert_ffn_bwd_ckpt, bwd)
+    args["ws"] = torch.empty(256, dtype=torch.uint8)
+    first = ("dw1", "dw2")  # they are asked for their type, and come before these two
+    for k, t in args.items():  # the others as addresses
+        rest = {n: v if n in first else 0x10000 for n, v in args.items()}
+        name = "dw1" if which == "backward" and k in ("dprob_perm", "ws", "dw2") else k
+        with pytest.raises(ValueError, match=f"{name} is on cpu"):
+            fn(s, **{**rest, k: t}, stream=0)
