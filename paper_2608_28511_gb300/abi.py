@@ -377,7 +377,12 @@ def _ckpt_rows(x, codes, scale):
         raise ValueError(f"codes {tuple(codes.shape)} {codes.dtype}: {(rows, cols)} int8 wanted")
     if scale.shape != (cols // 32, rows) or scale.dtype is not torch.float32:
         raise ValueError(f"scale {tuple(scale.shape)} {scale.dtype}: {(cols // 32, rows)} float32 wanted")
-    return _rows_dtype(x), rows, cols, x.stride(0) if rows > 1 else cols
+    dt, dev = _rows_dtype(x), x.get_device()
+    if dt >= 0 and (dev < 0 or codes.get_device() != dev or scale.get_device() != dev or
+                    dev != torch.cuda.current_device()):  # the library refuses other types
+        raise ValueError(f"x is on {x.device}, codes on {codes.device}, scale on {scale.device}: all on the current "
+                         "device wanted")
+    return dt, rows, cols, x.stride(0) if rows > 1 else cols
 
 
 def moe_ckpt_pack(x, codes, scale, stream=None):

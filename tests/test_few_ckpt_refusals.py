@@ -74,3 +74,12 @@ def test_ckpt_ffn_devices(L, which):
         name = "dw1" if which == "backward" and k in ("dprob_perm", "ws", "dw2") else k
         with pytest.raises(ValueError, match=f"{name} is on cpu"):
             fn(s, **{**rest, k: t}, stream=0)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_ckpt_rows_off_the_gpu(L, dt):
+    x, q, s = torch.zeros(4, 64, dtype=dt), torch.zeros(4, 64, dtype=torch.int8), torch.zeros(2, 4)
+    with pytest.raises(ValueError, match="is on cpu"):
+        L.moe_ckpt_pack(x, q, s, stream=0)
+    with pytest.raises(ValueError, match="is on cpu"):
+        L.moe_ckpt_unpack(q, s, x, stream=0)

@@ -34,3 +34,17 @@ def test_ffn_tensors_off_the_gpu():
         assert abi.moe_launch_count() == before
     torch.cuda.synchronize()
     assert abi.moe_check_device_status() == 0
+
+
+def test_rows_off_the_gpu():
+    from paper_2608_28511_gb300 import abi
+    x = torch.randn(4, 64, device="cuda")
+    q, s = torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.zeros(2, 4, device="cuda")
+    abi.moe_ckpt_pack(x, q, s)
+    before = abi.moe_launch_count()
+    for bad in ((x.cpu(), q, s), (x, q.cpu(), s), (x, q, s.cpu())):
+        with pytest.raises(ValueError, match="cpu"):
+            abi.moe_ckpt_pack(*bad)
+        with pytest.raises(ValueError, match="cpu"):
+            abi.moe_ckpt_unpack(bad[1], bad[2], bad[0])
+    assert abi.moe_launch_count() == before
