@@ -83,3 +83,11 @@ def test_ckpt_rows_off_the_gpu(L, dt):
         L.moe_ckpt_pack(x, q, s, stream=0)
     with pytest.raises(ValueError, match="is on cpu"):
         L.moe_ckpt_unpack(q, s, x, stream=0)
+
+
+def test_few_tokens_odd_rows_of_w1(L):
+    """w1 has gate and up rows in pairs; with 2F + 1 rows an expert's weights would be read a row off."""
+    from paper_2608_28511_gb300.layer import FewTokens
+    bf = torch.bfloat16
+    with pytest.raises(ValueError, match="w1"):
+        FewTokens(torch.zeros(8, 128, dtype=bf), torch.zeros(8, 129, 128, dtype=bf), torch.zeros(8, 128, 64, dtype=bf), 2)
