@@ -369,11 +369,12 @@ def _rows_dtype(t) -> int:
 def _ckpt_rows(x, codes, scale):
     """dtype, rows, cols, row pitch of x [rows, cols] (columns contiguous), checked against codes and scale."""
     torch = _torch or _t()
-    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
-        raise ValueError(f"x {tuple(x.shape)} with strides {tuple(x.stride())}: a matrix of rows that are contiguous "
-                         "and do not overlap wanted")
-    rows, cols = x.shape
-    if codes.shape != x.shape or codes.dtype is not torch.int8:
+    size, step = x.shape, x.stride()
+    if len(size) != 2 or (size[1] > 1 and step[1] != 1) or (size[0] > 1 and step[0] < size[1]):
+        raise ValueError(f"x {tuple(size)} with strides {step}: a matrix of rows that are contiguous and do not "
+                         "overlap wanted")
+    rows, cols = size
+    if codes.shape != size or codes.dtype is not torch.int8:
         raise ValueError(f"codes {tuple(codes.shape)} {codes.dtype}: {(rows, cols)} int8 wanted")
     if scale.shape != (cols // 32, rows) or scale.dtype is not torch.float32:
         raise ValueError(f"scale {tuple(scale.shape)} {scale.dtype}: {(cols // 32, rows)} float32 wanted")
@@ -382,7 +383,7 @@ def _ckpt_rows(x, codes, scale):
                     dev != torch.cuda.current_device()):  # the library refuses other types
         raise ValueError(f"x is on {x.device}, codes on {codes.device}, scale on {scale.device}: all on the current "
                          "device wanted")
-    return dt, rows, cols, x.stride(0) if rows > 1 else cols
+    return dt, rows, cols, step[0] if rows > 1 else cols
 
 
 def moe_ckpt_pack(x, codes, scale, stream=None):
@@ -410,19 +411,24 @@ def _any(name, t, *_):
 
 
 def _checked(fn):
-    """f(name, tensor, type, elements, width of the rows): the tensor's address, once it has these (a flat tensor
-    has no rows) and is on the current device, all of which the library cannot see.  With no type and number only
-    the device counts.  None and addresses pass."""
+    """f(name, tensor, type, shape): the tensor's address, once it has that type and shape (or is a flat or a
+    batched view of it) and is on the current device, all of which the library cannot see.  With no type only the
+    device counts.  None and addresses pass.  Attributes are read once each: a small call feels them (0.3 us a
+    tensor)."""
     at = None
 
-    def f(name, t, kind, n, width=None):
+    def f(name, t, kind, shape):
         nonlocal at
-        if t is None or isinstance(t, int):
-            return t
-        if n is not None and (t.dtype is not kind or t.numel() != n or
-                              (width is not None and t.size(-1) != width and t.dim() > 1)):
-            raise ValueError(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, not {n} elements" +
-                             (f" in rows of {width}" if width else "") + f" of {kind}")
+        try:
+            ok = t.dtype is kind and t.shape == shape
+        except AttributeError:
+            return _p(t)
+        if not ok and kind is not None:
+            n = 1
+            for d in shape:
+                n *= d
+            if t.dtype is not kind or t.numel() != n or (len(shape) > 1 and t.dim() > 1 and t.shape[-1] != shape[-1]):
+                raise ValueError(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, not {shape} of {kind}")
         dev = t.get_device()  # -1: not a GPU
         if dev != at:
             if dev < 0 or at is not None or dev != (_torch or _t()).cuda.current_device():
@@ -437,13 +443,13 @@ def _checked(fn):
 
 def moe_expert_ffn_ckpt(shape, x_perm, expert_offsets, w1, w2, h_q, h_scale, y_perm, ws, stream=None):
     torch = _torch or _t()
-    TK, D, E, F, bf = shape.T * shape.K, shape.D, shape.E, shape.F, torch.bfloat16
+    n, D, E, F, bf = shape.S * shape.GBS * shape.K, shape.D, shape.E, shape.F, torch.bfloat16
     p = _checked("moe_expert_ffn_ckpt") if shape.x_dtype == MOE_BF16 else _any  # the library refuses fp32
     _check("moe_expert_ffn_ckpt", lib().moe_expert_ffn_ckpt(
-        _shape(shape), p("x_perm", x_perm, bf, TK * D, D), p("expert_offsets", expert_offsets, torch.int32, E + 1),
-        p("w1", w1, bf, 2 * E * F * D, D), p("w2", w2, bf, E * D * F, F), p("h_q", h_q, torch.int8, 2 * TK * F, 2 * F),
-        p("h_scale", h_scale, torch.float32, TK * F // 16, TK), p("y_perm", y_perm, bf, TK * D, D),
-        p("ws", ws, None, None), _nbytes(ws), _stream(stream)))
+        _shape(shape), p("x_perm", x_perm, bf, (n, D)), p("expert_offsets", expert_offsets, torch.int32, (E + 1,)),
+        p("w1", w1, bf, (E, 2 * F, D)), p("w2", w2, bf, (E, D, F)), p("h_q", h_q, torch.int8, (n, 2 * F)),
+        p("h_scale", h_scale, torch.float32, (F // 16, n)), p("y_perm", y_perm, bf, (n, D)), p("ws", ws, None, None),
+        _nbytes(ws), _stream(stream)))
 
 
 def moe_expert_ffn_bwd_ckpt(shape, dy, x, prob_perm, row_of_slot, expert_offsets, h_q, h_scale, w1, w2, dx_perm, dw1,
@@ -453,17 +459,16 @@ def moe_expert_ffn_bwd_ckpt(shape, dy, x, prob_perm, row_of_slot, expert_offsets
     if dw != dw2.dtype:
         raise ValueError(f"dw1 is {dw}, dw2 {dw2.dtype}")
     torch = _torch or _t()
-    T, D, E, F = shape.T, shape.D, shape.E, shape.F
-    TK, n1, n2 = T * shape.K, 2 * E * F * D, E * D * F
-    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    T, K, D, E, F = shape.S * shape.GBS, shape.K, shape.D, shape.E, shape.F
+    n, bf, f32, i32 = T * K, torch.bfloat16, torch.float32, torch.int32
     p = _checked("moe_expert_ffn_bwd_ckpt") if shape.x_dtype == MOE_BF16 else _any
     _check("moe_expert_ffn_bwd_ckpt", lib().moe_expert_ffn_bwd_ckpt(
-        _shape(shape), p("dy", dy, bf, T * D, D), p("x", x, bf, T * D, D), p("prob_perm", prob_perm, f32, TK),
-        p("row_of_slot", row_of_slot, i32, TK), p("expert_offsets", expert_offsets, i32, E + 1),
-        p("h_q", h_q, torch.int8, 2 * TK * F, 2 * F), p("h_scale", h_scale, f32, TK * F // 16, TK),
-        p("w1", w1, bf, n1, D), p("w2", w2, bf, n2, F), p("dx_perm", dx_perm, bf, TK * D, D), _rows_dtype(dw1),
-        p("dw1", dw1, dw, n1, D), p("dw2", dw2, dw, n2, F), p("dprob_perm", dprob_perm, f32, TK),
-        p("ws", ws, None, None), _nbytes(ws), _stream(stream)))
+        _shape(shape), p("dy", dy, bf, (T, D)), p("x", x, bf, (T, D)), p("prob_perm", prob_perm, f32, (n,)),
+        p("row_of_slot", row_of_slot, i32, (n,)), p("expert_offsets", expert_offsets, i32, (E + 1,)),
+        p("h_q", h_q, torch.int8, (n, 2 * F)), p("h_scale", h_scale, f32, (F // 16, n)),
+        p("w1", w1, bf, (E, 2 * F, D)), p("w2", w2, bf, (E, D, F)), p("dx_perm", dx_perm, bf, (n, D)),
+        _rows_dtype(dw1), p("dw1", dw1, dw, (E, 2 * F, D)), p("dw2", dw2, dw, (E, D, F)),
+        p("dprob_perm", dprob_perm, f32, (n,)), p("ws", ws, None, None), _nbytes(ws), _stream(stream)))
 
 
 def moe_few_workspace_size(shape: MoeShape) -> int:
