@@ -413,12 +413,16 @@ int moe_expert_ffn_bwd_ckpt(const moe_shape_t* shape, const void* dy, const void
  *   y[t] = sum_k topk_prob[t, k] * (silu(g) * u) . w2_e^T, [g | u] = x[t] . w1_e^T,
  *   e = topk_idx[t, k]; fp32 accumulation, y rounded once.  silu(g) * u is the
  *   second product's operand: in bf16 it is two bf16 terms up to 32 tokens (no
- *   rounding that shows in y) and rounded once above.
+ *   rounding that shows in y, and no overflow before fp32's; only beside an
+ *   infinite w2 may their product be NaN where one term's is infinite) and
+ *   rounded once above.
  * x [T, D] is the experts' input and y [T, D] their output.  x_router [T, Din]
  * is the router's input; NULL means x (H = 0 only: a LatentMoE layer passes
  * its [T, H] input and runs its two projections around this call).  bias [E]
- * fp32 may be NULL.  Each chosen expert's weights are read once, whatever the
- * number of its tokens; results are bit-reproducible.  The second launch is
+ * fp32 may be NULL.  In bf16 each chosen expert's weights are read once, whatever
+ * the number of its tokens; in fp32 once for every eight of them.  The same batch
+ * gives the same bits; a token's last bits depend on the batch around it, whose
+ * size and experts decide how sums are cut.  The second launch is
  * cooperative (its blocks meet at bounded grid barriers).  Workspace:
  * moe_few_workspace_size(), of any contents; calls that may overlap need one
  * each. */

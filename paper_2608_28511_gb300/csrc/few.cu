@@ -5,9 +5,10 @@
 // Two launches.  few_router chooses every token's experts (and zeroes the
 // counters of the second launch's barriers).  few_layer (cooperative, one block
 // per SM): every block builds the row lists for itself (few.cuh), then the grid
-// computes act = silu(g) * u of every routed row, meets at a barrier, computes
-// W2 act by slot, meets again and combines.  fp32 runs on the CUDA cores
-// (here), bf16 on the tensor cores (few_tc.cu).
+// computes act = silu(g) * u of every routed row and W2 act by slot, meets at a
+// barrier and combines.  fp32 runs on the CUDA cores (here), with another barrier
+// between the products; bf16 on the tensor cores, with a counter an expert there
+// (few_tc.cu).
 #include <algorithm>
 
 #include "few.cuh"
@@ -45,8 +46,9 @@ template <typename T, int R, int NT, bool kWritten>  // kWritten: x was written 
 __device__ __forceinline__ void dot_rows(const uint4* const (&w)[R], const uint4* const (&x)[NT], int nvec, int lane,
                                          float (&acc)[R * NT]) {
   constexpr int NV = Vec<T>::N;
-  // steps in flight: as many as 128 registers hold (2 tokens of D = 1024, F = 512
-  // 27.1 us with two steps, 25.2 with four; 64 tokens 46.2 with two, 44.1 with one)
+  // steps in flight: as many as 128 registers hold (graph times; 2 tokens of D = 1024,
+  // F = 512, E = 64, K = 6: 27.0 us with two steps, 24.9 with four; 64 tokens of
+  // D = F = 512, E = 32, K = 4: 46.3 with two, 44.3 with one)
   constexpr int kSteps = NT <= 2 ? 4 : NT == 4 ? 2 : 1;
 #pragma unroll kSteps
   for (int v = lane; v < nvec; v += 32) {
@@ -317,7 +319,8 @@ __device__ __forceinline__ void second_unit(const Args& a, const Lists& L, const
 // D = F = 512, E = 64, K = 6 take 36.4 us as a graph, W1 at 6.2 and W2 at 6.4 TB/s,
 // the rest the router, two barriers and the combine.  The rows of weights are
 // split over warps and not over blocks, so every warp has loads of its own in
-// flight; 16 warps an SM (24 spill, 39.4 us; 12: 37.6).
+// flight; 16 warps an SM (24 spill, 39.4 us; 12: 37.6).  Experts with more than
+// eight tokens have their rows walked again for every eight of them.
 template <typename T>
 __global__ void __launch_bounds__(kSimtThreads, 1) few_layer_kernel(const __grid_constant__ Args a) {
   constexpr int NV = Vec<T>::N;

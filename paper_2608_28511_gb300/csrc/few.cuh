@@ -139,9 +139,10 @@ __device__ __forceinline__ void grid_barrier(uint32_t* counter, uint32_t* err) {
 }
 
 // bf16 keeps act as two terms up to 32 tokens: then y is rounded once, as from an
-// fp32 act, where one term adds about 40 % to its error. The second term's
-// rows and products cost 3 to 5 % of the time (7 tokens 53 -> 55 us); above 32
-// tokens its rows would take stages from the ring, and more.
+// fp32 act, where one term adds about 40 % to its error.  The second term's rows and
+// products cost 2 to 5 % of the time (graph: 1 token 31.7 -> 32.8 us, 7 tokens
+// 53.7 -> 54.8, 32 tokens of D = 2048, F = 1024, E = 64, K = 6 122.8 -> 129.4); above
+// 32 tokens its rows would take stages from the ring, and more.
 constexpr int kFewTerms(int T) { return T <= 32 ? 2 : 1; }
 
 // bf16, up to kSplitT tokens: a product with few tiles has them cut along k into

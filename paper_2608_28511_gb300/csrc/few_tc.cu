@@ -4,7 +4,7 @@
 // weight is read once by TMA and its 128 x 64 blocks feed tcgen05.mma straight
 // from a ring that fills the shared memory.  Bound by that stream from HBM: 128
 // tokens of D = 2048, F = 1024, E = 128, K = 8 read 1.6 GB in 251 us (graph, router
-// included), 6.9 TB/s while it runs; one token 100 MB in 34 us, of which about 16
+// included), 6.9 TB/s while it runs; one token 100 MB in 33 us, of which about 16
 // are the router, its launch, the lists, the first loads, the hand-over between
 // the products, the last barrier and the combine.
 //

@@ -425,9 +425,9 @@ class FewTokens:
         if (w_down is None) != (w_upp is None) or (w_s1 is None) != (w_s2 is None):
             raise ValueError("w_down goes with w_upp, and w_s1 with w_s2")
         Fs = w_s1.shape[0] if w_s1 is not None else 0
-        want = {"w_router": (w_router, (E, Din), dt), "w1": (w1, (E, 2 * F, D), dt),
-                "w2": (w2, (E, D, F), dt), "bias": (bias, (E,), torch.float32), "w_down": (w_down, (D, H), dt), "w_upp": (w_upp, (H, D), dt), "w_s1": (w_s1, (Fs, Din), dt),
-                "w_s2": (w_s2, (Din, Fs), dt)}
+        want = {"w_router": (w_router, (E, Din), dt), "w1": (w1, (E, 2 * F, D), dt), "w2": (w2, (E, D, F), dt),
+                "bias": (bias, (E,), torch.float32), "w_down": (w_down, (D, H), dt), "w_upp": (w_upp, (H, D), dt),
+                "w_s1": (w_s1, (Fs, Din), dt), "w_s2": (w_s2, (Din, Fs), dt)}
         for name, (t, size, kind) in want.items():
             if t is not None and (tuple(t.shape) != size or t.dtype != kind or t.device != w1.device):
                 raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}, not {size} {kind} on {w1.device}")
